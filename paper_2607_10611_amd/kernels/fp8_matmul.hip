@@ -179,14 +179,18 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte;
 // wave; p has `bytes` bytes.  The built-in function of this instruction makes
 // the compiler wait for it before any read of an LDS array that it may write,
 // which is every one here; written so, it waits where loads_done() says.  The
-// instruction writes no register.
+// instruction writes no register.  The compiler looks for hazards around an asm
+// block but not inside it: a scalar write of m0 needs one wait state before a load
+// to LDS reads it, hence the s_nop.  (The other such rule, five wait states from a
+// vector instruction's write of a scalar register to a load that reads it, holds
+// by distance; tests/test_isa_hazards.py checks both in the built library.)
 __device__ __forceinline__ void load_lds(const uint8_t* p, int64_t bytes, uint32_t lane_at,
                                          int at, uint32_t to) {
   const uint64_t base = (uint64_t)(uintptr_t)p;
   const i4v buffer = {(int)(uint32_t)base, (int)(uint32_t)(base >> 32) & 0xFFFF,
                       (int)(uint32_t)(bytes < 0xFFFFFFFFll ? bytes : 0xFFFFFFFFll), 0x00020000};
-  asm volatile("s_mov_b32 m0, %3\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
-               :: "v"(lane_at), "s"(buffer), "s"(at), "s"(to) : "m0", "memory");
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+               :: "v"(lane_at), "s"(buffer), "s"(at), "{m0}"(to) : "memory");
 }
 // Barrier behind which every wave's loads to LDS have arrived but its last KEEP
 // ones.

@@ -938,10 +938,14 @@ extern "C" int32_t madd_linear_fp8(const void* x, int32_t xfmt, int64_t ldx, con
   const uint64_t xb = xfmt == MADD_G_FP32 ? 4u : 2u, yb = yfmt == MADD_G_FP32 ? 4u : 2u;
   if (k > 0 && (!x || ldx < k || ldx > (int64_t)1 << 40)) return MADD_EINVAL;
   if ((uintptr_t)x & (xb - 1u)) return MADD_EALIGN;
-  const Range r[3] = {{k > 0 ? x : nullptr, xb * ((uint64_t)(m - 1) * (uint64_t)ldx + (uint64_t)k)},
-                      {y, yb * ((uint64_t)(m - 1) * (uint64_t)ldy + (uint64_t)n)},
+  // (above, the codes' place was one of the product's inputs, which may overlap)
+  const uint64_t un = (uint64_t)n, uk = (uint64_t)k;
+  const Range r[5] = {{k > 0 ? x : nullptr, xb * ((uint64_t)(m - 1) * (uint64_t)ldx + uk)},
+                      {b, un * uk},
+                      {bscale, un * uk / kFp8Block * (bscale_fmt == MADD_SCALE_FP16 ? 2u : 1u)},
+                      {y, yb * ((uint64_t)(m - 1) * (uint64_t)ldy + un)},
                       {workspace, (uint64_t)workspace_bytes}};
-  if (!writes_are_apart(r, 3, 1)) return MADD_EINVAL;
+  if (!writes_are_apart(r, 5, 3)) return MADD_EINVAL;
   if (one) {
     const bool sb16 = bscale_fmt == MADD_SCALE_FP16;
     const MatmulArgs p = {nullptr, nullptr, b, bscale, y, m, n, k / kFp8Block, ldy,

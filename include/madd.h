@@ -513,7 +513,9 @@ typedef struct madd_adamw_hparams {
  *           (madd_grad_norm's coefficient).  If it is a NaN the step changes
  *           nothing.
  * Arrays are aligned to their elements (else MADD_EALIGN) and start anywhere;
- * those of a tensor must not overlap (MADD_EINVAL; g and grad_scale may). */
+ * those of a tensor must not overlap (MADD_EINVAL; g and grad_scale may).  A
+ * tensor of more than (2^24 - 1) 2048 elements is MADD_EUNSUPPORTED.  Nothing is
+ * enqueued if an argument is refused. */
 int32_t madd_adamw_step(int32_t ntensors, void* const* w, int32_t wfmt, uint16_t* const* copy,
                         const void* const* g, int32_t gfmt, void* const* m, void* const* v,
                         uint8_t* const* scales, int32_t sfmt, const int64_t* numel,

@@ -456,6 +456,7 @@ __global__ __launch_bounds__(1024) void norm_final_kernel(const double* partial,
 // ---------------------------------------------------------------------------
 
 constexpr int64_t kMaxElements = (int64_t)1 << 60;
+constexpr int64_t kAdamMost = most_workgroups(kAdamThreads);  // of a launch, 3.4e10 elements
 
 typedef void (*adamw_fn)(AdamList, const float*);
 
@@ -569,7 +570,7 @@ int32_t madd_adamw_step(int32_t ntensors, void* const* w, int32_t wfmt, uint16_t
       return MADD_EALIGN;
     const int64_t whole = (n + kFp8Block - 1) / kFp8Block * kFp8Block;
     if (whole > INT64_MAX - index_base - total) return MADD_EINVAL;
-    if ((n + kAdamChunk - 1) / kAdamChunk > 0x7FFFFFFFll) return MADD_EUNSUPPORTED;
+    if ((n + kAdamChunk - 1) / kAdamChunk > kAdamMost) return MADD_EUNSUPPORTED;
     total += whole;
   }
   const bool sr = hp->rounding == MADD_ROUND_SR;
@@ -592,7 +593,7 @@ int32_t madd_adamw_step(int32_t ntensors, void* const* w, int32_t wfmt, uint16_t
     const int64_t n = numel[i];
     if (n == 0) continue;
     const int64_t nch = (n + kAdamChunk - 1) / kAdamChunk;
-    if (l.count == kAdamList || chunks + nch > 0x7FFFFFFFll) {
+    if (l.count == kAdamList || chunks + nch > kAdamMost) {
       rc = flush();
       if (rc != MADD_OK) return rc;
     }

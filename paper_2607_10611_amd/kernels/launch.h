@@ -20,11 +20,14 @@ template <typename Tuple, size_t... I>
 inline void kernel_args(void** argv, Tuple& t, std::index_sequence<I...>) {
   ((argv[I] = (void*)&std::get<I>(t)), ...);
 }
+
+// Workgroups of `threads` threads that a launch holds: fewer than 2^32 threads.
+constexpr int64_t most_workgroups(int64_t threads) { return 0xFFFFFFFFll / threads; }
+
 template <typename... P, typename... A>
 inline int32_t launch_kernel_lds(void (*k)(P...), dim3 grid, dim3 block, unsigned lds,
                                  hipStream_t stream, A&&... a) {
-  // more threads than a launch holds
-  if ((uint64_t)grid.x * block.x > 0xFFFFFFFFull) return MADD_EUNSUPPORTED;
+  if ((int64_t)grid.x > most_workgroups(block.x)) return MADD_EUNSUPPORTED;
   std::tuple<P...> args(std::forward<A>(a)...);
   void* argv[sizeof...(P) > 0 ? sizeof...(P) : 1];
   kernel_args(argv, args, std::index_sequence_for<P...>{});

@@ -1,10 +1,12 @@
 """What the FP8 and AdamW entry points refuse, before any device work (CPU)."""
+import ctypes
+
 import test_abi
 from paper_2607_10611_amd import binding as B
 
 fake_addresses = test_abi.fake_addresses  # made-up device addresses: CPU only
 X_, B_, SB_, Y_, WS_ = (0x1000000 * (k + 1) for k in range(5))
-EINVAL, EUNSUPPORTED = -1, -3
+EINVAL, EUNSUPPORTED, EDEVICE = -1, -3, -4
 
 
 def linear(m=50, n=70, k=256, x=X_, b=B_, sb=SB_, y=Y_, ws=WS_, wsb=None, ldx=None):
@@ -22,3 +24,31 @@ def test_linear_refuses_weights_in_its_workspace():
     for bad in (dict(b=WS_), dict(b=WS_ + 16), dict(b=WS_ - 16), dict(b=WS_ + need - 16),
                 dict(sb=WS_), dict(sb=WS_ + 64), dict(sb=WS_ - 2), dict(sb=WS_ + need - 2)):
         assert linear(**bad) == EINVAL, bad
+
+
+def _adamw(sizes):
+    """madd_adamw_step of bf16 weights, bf16 gradients and 8-bit states at made-up
+    addresses, 2^42 bytes apart."""
+    k = len(sizes)
+    at = lambda j: ctypes.cast((ctypes.c_void_p * k)(  # noqa: E731
+        *[((6 * i + j + 1) << 42) for i in range(k)]), ctypes.POINTER(ctypes.c_void_p))
+    h = B._adamw_hp(dict(lr=1e-3, step=1))
+    return B.lib().madd_adamw_step(k, at(0), 0, None, at(1), 1, at(2), at(3), at(4), 1,
+                                   (ctypes.c_int64 * k)(*sizes), 0, ctypes.byref(h), None, None)
+
+
+@fake_addresses
+def test_adamw_refuses_a_tensor_that_no_launch_holds_before_the_first():
+    """A tensor of more workgroups than a launch holds is refused before any other
+    tensor of the list is stepped.  (Without a device a launch ends in MADD_EDEVICE.)"""
+    most = (2 ** 24 - 1) * 2048
+    assert _adamw([1000] * 60 + [most + 1]) == EUNSUPPORTED
+    assert _adamw([most + 1]) == EUNSUPPORTED
+    assert _adamw([most]) == EDEVICE and _adamw([1000]) == EDEVICE
+
+
+@fake_addresses
+def test_adamw_splits_lists_that_no_launch_holds():
+    """Tensors that fit a launch each but not together take several launches."""
+    half = 2 ** 23 * 2048
+    assert _adamw([half, half, half]) == EDEVICE  # a launch was tried, none was refused

@@ -809,17 +809,36 @@ int32_t run(const MatmulArgs& p, const Plan& how, hipStream_t stream) {
   else return launch_tiles<AF, BF, false, 2, 2, 2, 2, 2>(p, how.parts, stream);
 }
 
+// The plan for these sizes, or false if a launch of it would hold too many workgroups
+// or an offset that the kernels count in 32 bits would not fit.
+bool plan_launches(int64_t m, int64_t n, int64_t kb, bool sb16, int64_t workspace, Plan* how) {
+  *how = plan(m, n, kb, sb16, workspace);
+  auto fits = [&](int64_t rows, int64_t cols, int64_t threads, bool flat) {
+    const int64_t down = (m + rows - 1) / rows, across = (n + cols - 1) / cols;
+    return across <= most_workgroups(threads) / (flat ? down : 1);  // flat: both in grid.x
+  };
+  const bool join = how->parts == 1 || m * ((n + 3) / 4) <= most_workgroups(256) * 256;
+  if (kb > 0xFFFF || !join) return false;
+  switch (how->way) {
+    case kRows16: return fits(16, 16, 512, false);
+    case kRows32: return fits(32, 32, 512, false);
+    case kRows64: return fits(64, 32, 512, false);
+    case kTile64: return fits(64, 256, 256, true);
+    case kTile128: return fits(128, 128, 256, true);
+    default: return sb16 ? fits(256, 128, 512, true) : fits(256, 256, 256, true);
+  }
+}
+
 template <int AF, int BF>
 int32_t matmul(const MatmulArgs& whole, bool sb16, void* workspace, int64_t bytes,
                hipStream_t stream) {
-  Plan how = plan(whole.m, whole.n, whole.kb, sb16, workspace ? bytes : 0);
+  Plan how;
+  if (!plan_launches(whole.m, whole.n, whole.kb, sb16, workspace ? bytes : 0, &how))
+    return MADD_EUNSUPPORTED;
   MatmulArgs p = whole;
   p.per = (int32_t)((p.kb + how.parts - 1) / how.parts);
   if (p.per > 0) how.parts = (p.kb + p.per - 1) / p.per;  // none empty
   p.part = 0;
-  // (the largest grids and offsets that the kernels count in 32 bits)
-  if ((p.m + 63) / 64 * ((p.n + 127) / 128) > 0x7FFFFFFFll || p.kb > 0xFFFF)
-    return MADD_EUNSUPPORTED;
   if (how.parts > 1) {
     p.c = workspace;
     p.ldc = p.n;
@@ -958,6 +977,10 @@ extern "C" int32_t madd_linear_fp8(const void* x, int32_t xfmt, int64_t ldx, con
     return sb16 ? linear_rows<WF_E5M2, true>(p, raw, xfmt, st)
                 : linear_rows<WF_E5M2, false>(p, raw, xfmt, st);
   }
+  Plan how;
+  if (!plan_launches(m, n, k / kFp8Block, bscale_fmt == MADD_SCALE_FP16, workspace_bytes - codes,
+                     &how))
+    return MADD_EUNSUPPORTED;
   rc = madd_quantize_fp8(x, xfmt, m, k, ldx, MADD_W_FP8_E4M3, q, s, nullptr, nullptr, stream);
   if (rc != MADD_OK) return rc;
   return madd_matmul_fp8(q, MADD_W_FP8_E4M3, s, b, bfmt, bscale, bscale_fmt, y, yfmt, ldy, 0, m, n,

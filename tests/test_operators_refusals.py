@@ -52,3 +52,17 @@ def test_adamw_splits_lists_that_no_launch_holds():
     """Tensors that fit a launch each but not together take several launches."""
     half = 2 ** 23 * 2048
     assert _adamw([half, half, half]) == EDEVICE  # a launch was tried, none was refused
+
+
+@fake_addresses
+def test_linear_refuses_what_no_launch_holds_before_the_first():
+    """Sizes that the product cannot take are refused before x is quantized.
+    (Without a device a launch ends in MADD_EDEVICE.)"""
+    far = {name: (j + 1) << 45 for j, name in enumerate(("x", "b", "sb", "y", "ws"))}
+    assert linear(m=50, n=70, k=128 * 65536, **far) == EUNSUPPORTED
+    assert linear(m=50, n=70, k=128 * 65535, **far) == EDEVICE
+    for m in (17, 3000):
+        assert linear(m=m, n=2 ** 31, k=128, **far) == EUNSUPPORTED, m
+    assert linear(m=40, n=2 ** 31, k=128, **far) == EDEVICE  # 2^23 tiles of 64x256
+    for m in (17, 40, 3000):
+        assert linear(m=m, n=2 ** 20, k=128, **far) == EDEVICE, m

@@ -899,6 +899,7 @@ static int32_t check_matmul(const uint8_t* a, int32_t afmt, const uint8_t* ascal
   if (((uintptr_t)a & 15u) || ((uintptr_t)b & 15u) || ((uintptr_t)c & (cb - 1u)) ||
       ((uintptr_t)workspace & 15u) || (sb16 && ((uintptr_t)bscale & 1u)))
     return MADD_EALIGN;
+  if (!rows_fit(m, ldc, (int64_t)cb)) return MADD_EINVAL;
   const uint64_t um = (uint64_t)m, un = (uint64_t)n, uk = (uint64_t)k;
   const Range r[6] = {{a, um * uk}, {ascale, um * uk / kFp8Block}, {b, un * uk},
                       {bscale, un * uk / kFp8Block * (sb16 ? 2u : 1u)},
@@ -955,7 +956,8 @@ extern "C" int32_t madd_linear_fp8(const void* x, int32_t xfmt, int64_t ldx, con
   if (rc != MADD_OK || m == 0 || n == 0) return rc;
   if (xfmt != MADD_G_FP32 && xfmt != MADD_G_BF16) return MADD_EINVAL;
   const uint64_t xb = xfmt == MADD_G_FP32 ? 4u : 2u, yb = yfmt == MADD_G_FP32 ? 4u : 2u;
-  if (k > 0 && (!x || ldx < k || ldx > (int64_t)1 << 40)) return MADD_EINVAL;
+  if (k > 0 && (!x || ldx < k || ldx > (int64_t)1 << 40 || !rows_fit(m, ldx, (int64_t)xb)))
+    return MADD_EINVAL;
   if ((uintptr_t)x & (xb - 1u)) return MADD_EALIGN;
   // (above, the codes' place was one of the product's inputs, which may overlap)
   const uint64_t un = (uint64_t)n, uk = (uint64_t)k;

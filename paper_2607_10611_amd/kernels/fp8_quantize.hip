@@ -238,6 +238,7 @@ extern "C" int32_t madd_quantize_fp8(const void* x, int32_t xfmt, int64_t rows, 
   if ((!q && !qt) || !q != !qscale || !qt != !qtscale) return MADD_EINVAL;
   if (!x || ldx < cols || ldx > (int64_t)1 << 40) return MADD_EINVAL;
   const uint64_t xb = xfmt == MADD_G_FP32 ? 4u : 2u;
+  if (!rows_fit(rows, ldx, (int64_t)xb)) return MADD_EINVAL;
   if ((uintptr_t)x & (xb - 1u)) return MADD_EALIGN;
   if (((uintptr_t)q & 15u) || ((uintptr_t)qt & 15u)) return MADD_EALIGN;
   const uint64_t r = (uint64_t)rows, c = (uint64_t)cols;

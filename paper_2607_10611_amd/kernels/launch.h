@@ -42,6 +42,12 @@ inline int32_t launch_kernel(void (*k)(P...), dim3 grid, dim3 block, hipStream_t
   return launch_kernel_lds(k, grid, block, 0u, stream, std::forward<A>(a)...);
 }
 
+// Whether a matrix of rows `ld` elements apart ends within 2^57 bytes, the addresses
+// that there are (so that its offsets and the ranges below do not wrap round).
+inline bool rows_fit(int64_t rows, int64_t ld, int64_t bytes) {
+  return rows <= 1 || ld <= 0 || rows - 1 <= ((int64_t)1 << 57) / bytes / ld;
+}
+
 // A byte range of device memory that a call reads or writes.
 struct Range {
   const void* p;

@@ -66,3 +66,26 @@ def test_linear_refuses_what_no_launch_holds_before_the_first():
     assert linear(m=40, n=2 ** 31, k=128, **far) == EDEVICE  # 2^23 tiles of 64x256
     for m in (17, 40, 3000):
         assert linear(m=m, n=2 ** 20, k=128, **far) == EDEVICE, m
+
+
+@fake_addresses
+def test_matrices_past_the_end_of_memory_are_refused():
+    """Row strides that 64-bit offsets cannot follow: the ranges of such matrices would
+    wrap round in the checks for overlap."""
+    lib, far = B.lib(), [(j + 1) << 45 for j in range(5)]
+    rows, ld = 2 ** 31, 2 ** 40
+
+    def matmul(ldc):
+        return lib.madd_matmul_fp8(far[0], 1, far[1], far[2], 1, far[3], 0, far[4], 0, ldc, 0,
+                                   rows, 70, 128, None, 0, None)
+
+    def quantize(ldx):
+        return lib.madd_quantize_fp8(far[0], 1, rows, 128, ldx, 1, far[1], far[2], None, None,
+                                     None)
+
+    assert matmul(ld) == EINVAL and quantize(ld) == EINVAL
+    assert linear(m=3, n=70, k=128, ldx=2 ** 41) == EINVAL
+    ws = lib.madd_linear_fp8_workspace(rows, 70, 128)
+    assert linear(m=rows, n=70, k=128, x=far[0], b=far[1], sb=far[2], y=far[3], ws=far[4] << 4,
+                  wsb=ws, ldx=ld) == EINVAL
+    assert quantize(128) == EDEVICE

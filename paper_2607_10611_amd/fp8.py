@@ -189,6 +189,7 @@ class _Linear(torch.autograd.Function):
         return y
 
     @staticmethod
+    @torch.autograd.function.once_differentiable  # autograd does not see into the kernels
     def backward(ctx, dy):
         copy, q, s = ctx.saved_tensors
         need_dx, need_dw = ctx.needs_input_grad[0], ctx.needs_input_grad[1]

@@ -1,0 +1,86 @@
+"""FP8Linear and its autograd function on the CPU, the kernels' calls replaced by
+torch operations (what is tested is which of them run, and what autograd sees)."""
+import pytest
+import torch
+
+from paper_2607_10611_amd import fp8
+
+
+def values(m):
+    return m.dequantize(torch.float64)
+
+
+def quantize(x, fmt="e4m3", rows=True, cols=False):
+    """Codes that keep small integers, with scale 1."""
+    def blocks(t):
+        t = torch.nn.functional.pad(t.detach().float(), (0, -t.shape[1] % 128))
+        q = t.to(fp8._DTYPE[fmt])
+        return fp8.BlockMatrix(q, torch.full((q.shape[0], q.shape[1] // 128), 127,
+                                             dtype=torch.uint8))
+    x = x.reshape(-1, x.shape[-1])
+    r, c = (blocks(x) if rows else None), (blocks(x.t().contiguous()) if cols else None)
+    for m, n in ((r, x.shape[1]), (c, x.shape[0])):
+        if m is not None:
+            m.cols = n
+    return r, c
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Names of the calls made, in order."""
+    made = []
+
+    def matmul(a, b, dtype=torch.bfloat16, out=None, accumulate=False):
+        made.append("matmul")
+        k = min(a.codes.shape[1], b.codes.shape[1])
+        full = lambda m: fp8.BlockMatrix(m.codes, m.scales, m.fmt).dequantize(torch.float64)  # noqa: E731
+        return (full(a)[:, :k] @ full(b)[:, :k].t()).to(dtype)
+
+    def linear(x, w, dtype=torch.bfloat16, out=None):
+        made.append("linear")
+        y = matmul(quantize(x)[0], w, dtype)
+        made.pop()
+        return y.view(*x.shape[:-1], y.shape[1])
+
+    def counted(*a, **kw):
+        made.append("quantize")
+        return quantize(*a, **kw)
+
+    monkeypatch.setattr(fp8, "quantize", counted)
+    monkeypatch.setattr(fp8, "matmul", matmul)
+    monkeypatch.setattr(fp8, "linear", linear)
+    return made
+
+
+def integers(*shape, seed=0, dtype=torch.bfloat16):
+    gen = torch.Generator().manual_seed(seed)
+    return torch.randint(-3, 4, shape, generator=gen).to(dtype)
+
+
+def layer(k=128, n=6, master=True):
+    lin = fp8.FP8Linear(k, n)
+    with torch.no_grad():
+        lin.weight.copy_(integers(n, k, seed=1))
+    if master:
+        m = quantize(lin.weight)[0]
+        s = torch.ones(n * k // 128, dtype=torch.float16)
+        lin.use_master(m.codes.view(torch.uint8).view(-1), s)
+    return lin
+
+
+def test_first_derivatives(calls):
+    lin, x = layer(), integers(4, 128, seed=2).requires_grad_()
+    dy = integers(4, 6, seed=3)
+    lin(x).backward(dy)
+    assert torch.equal(x.grad.double(), dy.double() @ lin.weight.detach().double())
+    assert torch.equal(lin.weight.grad.double(), dy.double().t() @ x.detach().double())
+
+
+def test_second_derivatives_are_refused(calls):
+    """The backward pass runs in kernels that autograd does not see: a second
+    derivative through it would silently be without its terms."""
+    lin, x = layer(), integers(4, 128, seed=2).requires_grad_()
+    loss = lin(x).float().square().sum() + x.float().pow(3).sum()
+    (dx,) = torch.autograd.grad(loss, x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dx.float().sum().backward()

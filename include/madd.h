@@ -479,7 +479,8 @@ int32_t madd_linear_fp8(const void* x, int32_t xfmt, int64_t ldx, const uint8_t*
  *          value gets the NaN scale and zero payloads. */
 typedef enum madd_adamw_state { MADD_A_FP32 = 0, MADD_A_8BIT = 1 } madd_adamw_state;
 
-/* Hyper-parameters of one AdamW step.  Valid: 0 <= beta1 < 1, 0 <= beta2 < 1,
+/* Hyper-parameters of one AdamW step, read at the call: one captured in a graph
+ * replays with the step number that it was captured with.  Valid: 0 <= beta1 < 1, 0 <= beta2 < 1,
  * eps >= 0, lr and weight_decay finite, rounding a madd_round (of bf16
  * weights), 1 <= step <= 2^32 - 1 (else MADD_EINVAL). */
 typedef struct madd_adamw_hparams {

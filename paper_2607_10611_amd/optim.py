@@ -453,7 +453,11 @@ class AdamW(torch.optim.Optimizer):
     def step(self, closure=None, grad_scale=None):
         """One step.  grad_scale: a float32 GPU tensor of one value that
         multiplies every gradient on the way (grad_norm's coefficient); a NaN
-        leaves parameters and states as they are."""
+        leaves parameters and states as they are.  A step cannot be captured in a
+        graph: its number and hyper-parameters go to the kernel by value."""
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("AdamW: a step cannot be captured (every replay would repeat its "
+                               "step number)")
         loss = None
         if closure is not None:
             with torch.enable_grad():

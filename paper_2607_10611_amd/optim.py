@@ -470,6 +470,8 @@ class AdamW(torch.optim.Optimizer):
                           weight_decay=group["weight_decay"], rounding=group["rounding"],
                           seed=group["seed"], step=t + 1)
                 B.madd_adamw_step(al, hp, grad_scale=grad_scale, index_base=self._base[run[0]])
+                # the kernel writes through addresses, which autograd does not see
+                torch.autograd.graph.increment_version(run)
                 # the launch is ordered on the current stream: the gradients
                 # need no reference past it
                 al.grads.set([None] * al.n)

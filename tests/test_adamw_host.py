@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2607_10611_amd import binding as B
 from paper_2607_10611_amd.optim import AdamW
 
 
@@ -21,3 +22,29 @@ def test_a_captured_step_is_refused(monkeypatch):
     with pytest.raises(RuntimeError, match="captur"):
         opt.step()
     assert not opt.state[p]
+
+
+@pytest.fixture
+def stub(monkeypatch):
+    """AdamW whose checks take CPU tensors and whose kernel call does nothing; the list
+    of the (hyper-parameters, grad_scale) that it was called with."""
+    made = []
+    monkeypatch.setattr(AdamW, "_check_param", staticmethod(lambda p, master: None))
+    monkeypatch.setattr(B, "_need", lambda *a: None)
+    monkeypatch.setattr(B, "madd_adamw_step",
+                        lambda al, hp, grad_scale=None, index_base=0: made.append((hp, grad_scale)))
+    return made
+
+
+def test_a_step_tells_autograd_that_the_parameters_changed(stub):
+    """A backward pass through tensors saved before the step raises, as after torch's
+    own optimizers, instead of using the new values."""
+    w, other = parameter(), parameter()
+    other.grad = None
+    x = torch.ones(4, requires_grad=True)
+    loss, loss2 = (x * w).sum(), (x * other).sum()
+    AdamW([w, other]).step()
+    assert len(stub) == 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    loss2.backward()  # a parameter that had no gradient is as it was

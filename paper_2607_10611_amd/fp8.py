@@ -26,6 +26,7 @@ from functools import lru_cache
 import torch
 
 from . import binding as B
+from .optim import was_replaced
 
 _FMT = {torch.float8_e4m3fn: "e4m3", torch.float8_e5m2: "e5m2"}
 _DTYPE = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
@@ -218,16 +219,27 @@ class FP8Linear(torch.nn.Module):
         w = torch.randn(out_features, in_features, device=device) * in_features ** -0.5
         self.weight = torch.nn.Parameter(w.to(torch.bfloat16))
         self.grad_fmt = grad_fmt
-        self._master = None
+        self._master = self._given = None
 
     def use_master(self, codes, scales, fmt: str = "e4m3"):
         """Run the forward pass on this block-scaled master (its storage is read
-        at every call, so the optimizer's in-place updates are seen)."""
+        at every call, so the optimizer's in-place updates are seen).  After
+        MAdam.load_state_dict, which replaces the state's tensors, call it again:
+        until then the forward pass raises.  Loading the layer's own weight from a
+        state dict ends it, and the weight is read again."""
         w = BlockMatrix(codes, scales.view(torch.int16), fmt, shape=self.weight.shape)
-        self._master = (w.codes, w.scales, fmt)
+        self._master, self._given = (w.codes, w.scales, fmt), (codes, scales)
+
+    def _load_from_state_dict(self, state_dict, prefix, *args, **kwargs):
+        super()._load_from_state_dict(state_dict, prefix, *args, **kwargs)
+        if prefix + "weight" in state_dict:
+            self._master = self._given = None
 
     def forward(self, x):
         if self._master is not None:
+            if any(map(was_replaced, self._given)):
+                raise RuntimeError("FP8Linear: the optimizer has replaced this master "
+                                   "(load_state_dict); call use_master with the new one")
             codes, scales, fmt = self._master
         else:
             w = quantize(self.weight.detach(), "e4m3")[0]

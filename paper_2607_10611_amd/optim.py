@@ -24,6 +24,7 @@ import math
 from collections import OrderedDict
 
 import torch
+from torch.utils.weak import WeakIdKeyDictionary
 
 from . import binding as B
 
@@ -38,8 +39,16 @@ _STATES = {"fp32": torch.float32, "bf16": torch.int16, "bf16_sr": torch.int16}
 _MASTERS = {"e4m3": 128, "e5m2": 128, "mxfp4": B.MX_BLOCK, "nvfp4": B.NV_BLOCK,
             "nvfp4_current": B.NV_BLOCK}
 _SAVED = ("m", "v", "ve", "q", "scales")  # state tensors whose dtype and bits are kept
+# master codes and scales that load_state_dict replaced, while anything still holds them
+_replaced = WeakIdKeyDictionary()
 _HP_KEYS = ("lr_add", "lr_mul", "eps", "tau", "r_max", "eps0", "g_max", "d_mult_max", "w_max",
             "rounding", "seed")
+
+
+def was_replaced(t) -> bool:
+    """Whether t is, or is a view of, master codes or scales that are no longer
+    an optimizer's because MAdam.load_state_dict put others in their place."""
+    return t in _replaced or (t._base is not None and t._base in _replaced)
 
 
 class MAdam(torch.optim.Optimizer):
@@ -116,10 +125,15 @@ class MAdam(torch.optim.Optimizer):
     def load_state_dict(self, state_dict):
         """As torch.optim.Optimizer's, except that the moments and any master
         codes and scales keep the dtype and bits they were saved with (the
-        base class casts every state tensor to its parameter's dtype)."""
+        base class casts every state tensor to its parameter's dtype).  The
+        state's tensors are new ones: a layer that reads a master needs the
+        new one (FP8Linear.use_master)."""
         from itertools import chain
         saved = state_dict["state"]
+        masters = [st[k] for st in self.state.values() for k in ("q", "scales") if k in st]
         super().load_state_dict(state_dict)
+        for t in masters:
+            _replaced[t] = True
         ids = chain.from_iterable(g["params"] for g in state_dict["param_groups"])
         params = chain.from_iterable(g["params"] for g in self.param_groups)
         for pid, p in zip(ids, params):

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2607_10611_amd import fp8
+from paper_2607_10611_amd.optim import MAdam
 
 
 def values(m):
@@ -84,3 +85,43 @@ def test_second_derivatives_are_refused(calls):
     (dx,) = torch.autograd.grad(loss, x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         dx.float().sum().backward()
+
+
+def with_optimizer(lin):
+    """MAdam over the layer's weight, its state as a first step leaves it."""
+    opt, n = MAdam([lin.weight], master_format="e4m3"), lin.weight.numel()
+    state = lambda *s, dtype=torch.uint8: torch.ones(*s, dtype=dtype)  # noqa: E731
+    opt.state[lin.weight] = dict(step=1, m=state(n, dtype=torch.float32),
+                                 v=state(n, dtype=torch.float32),
+                                 ve=state(n, dtype=torch.float32), q=state(n),
+                                 scales=state(n // 64))
+    return opt, opt.state[lin.weight]
+
+
+@pytest.mark.parametrize("shaped", [False, True])
+def test_a_master_that_the_optimizer_replaced_is_not_read(calls, shaped):
+    """MAdam.load_state_dict puts new tensors in place of the state's: a layer that
+    still held the old ones would read a master that no step updates."""
+    lin = layer(master=False)
+    opt, st = with_optimizer(lin)
+    lin.use_master(st["q"].view(6, 128) if shaped else st["q"], st["scales"])
+    saved = opt.state_dict()
+    y = lin(integers(2, 128))
+    opt.load_state_dict(saved)
+    with pytest.raises(RuntimeError, match="use_master"):
+        lin(integers(2, 128))
+    st = opt.state[lin.weight]
+    lin.use_master(st["q"], st["scales"])
+    assert torch.equal(lin(integers(2, 128)), y)
+    assert torch.equal(saved["state"][0]["q"], st["q"])  # the saved state is as it was
+
+
+def test_a_layer_whose_weight_is_loaded_reads_that_weight(calls):
+    """The master is another weight's then."""
+    lin, other = layer(), layer(master=False)
+    x = integers(3, 128, seed=4)
+    with torch.no_grad():
+        other.weight.neg_()
+    assert torch.equal(lin(x), -other(x))
+    torch.nn.ModuleDict(dict(a=lin)).load_state_dict({"a.weight": other.weight})
+    assert torch.equal(lin(x), other(x))

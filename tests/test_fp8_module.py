@@ -125,3 +125,30 @@ def test_a_layer_whose_weight_is_loaded_reads_that_weight(calls):
     assert torch.equal(lin(x), -other(x))
     torch.nn.ModuleDict(dict(a=lin)).load_state_dict({"a.weight": other.weight})
     assert torch.equal(lin(x), other(x))
+
+
+def test_reading_the_model_takes_the_serving_path(calls):
+    """No gradient is wanted: x W^T alone runs, and x's column blocks, which only the
+    weight's gradient needs, are not made."""
+    lin, x = layer(), integers(4, 128, seed=2)
+    want = lin(x).detach()
+    assert calls == ["quantize", "matmul"]
+    for mode in (torch.no_grad, torch.inference_mode):
+        calls.clear()
+        with mode():
+            y = lin(x)
+        assert calls == ["linear"] and torch.equal(y, want) and not y.requires_grad
+    lin.weight.requires_grad_(False)
+    calls.clear()
+    assert torch.equal(lin(x), want) and calls == ["linear"]
+
+
+def test_a_frozen_weight_passes_gradients_on(calls):
+    lin, x = layer(), integers(4, 128, seed=2).requires_grad_()
+    lin.weight.requires_grad_(False)
+    dy = integers(4, 6, seed=3)
+    y = lin(x)
+    assert calls == ["linear"]
+    y.backward(dy)
+    assert torch.equal(x.grad.double(), dy.double() @ lin.weight.double())
+    assert lin.weight.grad is None

@@ -63,8 +63,10 @@ class BlockMatrix:
             raise ValueError("BlockMatrix: codes and scales must be contiguous")
         if scales.dim() != 2:
             scales = scales.view(rows, blocks)
-        self.codes, self.scales, self.fmt = codes, scales, fmt
-        self.cols = k if cols is None else cols
+        cols = k if cols is None else cols
+        if not max(k - B.FP8_BLOCK, 0) < cols <= k and not cols == k == 0:
+            raise ValueError(f"BlockMatrix: cols must end in the last block of {k} (got {cols})")
+        self.codes, self.scales, self.fmt, self.cols = codes, scales, fmt, cols
 
     @classmethod
     def _made(cls, codes, scales, fmt: str, cols: int):
@@ -135,6 +137,8 @@ def matmul(a: BlockMatrix, b: BlockMatrix, dtype=torch.bfloat16, out=None,
     with ``accumulate``).  a's scales must be E8M0."""
     if accumulate and out is None:
         raise ValueError("matmul: accumulate needs out")
+    if a.cols != b.cols:
+        raise ValueError(f"matmul: operands of {a.cols} and {b.cols} columns")
     m, n, k = a.codes.shape[0], b.codes.shape[0], a.codes.shape[1]
     if out is None:
         out = torch.empty(m, n, dtype=dtype, device=a.codes.device)
@@ -144,9 +148,12 @@ def matmul(a: BlockMatrix, b: BlockMatrix, dtype=torch.bfloat16, out=None,
 
 
 def linear(x, w: BlockMatrix, dtype=torch.bfloat16, out=None):
-    """x W^T: x (..., k) bf16 or fp32, quantized to E4M3 rows on the way."""
+    """x W^T: x (..., k) bf16 or fp32, k a multiple of 128, quantized to E4M3 rows
+    on the way."""
     a = _as_matrix(x)
     (n, k), m, device = w.codes.shape, a.shape[0], x.device
+    if a.shape[1] != w.cols:
+        raise ValueError(f"linear: x and the weights have {a.shape[1]} and {w.cols} columns")
     y = torch.empty(m, n, dtype=dtype, device=device) if out is None else out
     B.madd_linear_fp8(a, w.codes, w.fmt, w.scales, y, _workspace("linear", m, n, k, device))
     return y if out is not None or x.dim() == 2 else y.view(*x.shape[:-1], n)

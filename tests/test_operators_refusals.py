@@ -1,8 +1,12 @@
 """What the FP8 and AdamW entry points refuse, before any device work (CPU)."""
 import ctypes
 
+import pytest
+import torch
+
 import test_abi
 from paper_2607_10611_amd import binding as B
+from paper_2607_10611_amd import fp8
 
 fake_addresses = test_abi.fake_addresses  # made-up device addresses: CPU only
 X_, B_, SB_, Y_, WS_ = (0x1000000 * (k + 1) for k in range(5))
@@ -89,3 +93,37 @@ def test_matrices_past_the_end_of_memory_are_refused():
     assert linear(m=rows, n=70, k=128, x=far[0], b=far[1], sb=far[2], y=far[3], ws=far[4] << 4,
                   wsb=ws, ldx=ld) == EINVAL
     assert quantize(128) == EDEVICE
+
+
+def _blocks(rows, cols, **kw):
+    k = -(-cols // 128) * 128
+    return fp8.BlockMatrix(torch.zeros(rows, k, dtype=torch.uint8),
+                           torch.zeros(rows, k // 128, dtype=torch.uint8), "e4m3", cols=cols, **kw)
+
+
+def test_lengths_that_differ_within_a_block_are_refused(monkeypatch):
+    """Operands whose padded rows are as long but which count different numbers of
+    columns: the product would silently take the padding of one for zeros of the other."""
+    monkeypatch.setattr(B, "madd_matmul_fp8", lambda *a: pytest.fail("reached the kernel"))
+    monkeypatch.setattr(B, "madd_linear_fp8", lambda *a: pytest.fail("reached the kernel"))
+    monkeypatch.setattr(B, "madd_quantize_fp8", lambda *a: None)
+    x = lambda *s: torch.zeros(*s)  # noqa: E731
+    with pytest.raises(ValueError, match="columns"):
+        fp8.matmul(_blocks(3, 100), _blocks(4, 128))
+    with pytest.raises(ValueError, match="columns"):
+        fp8.linear(x(3, 128), _blocks(4, 100))
+    with pytest.raises(ValueError, match="columns"):
+        fp8.linear_forward(x(3, 100), _blocks(4, 128))
+    xt, copy = _blocks(256, 40), x(70, 256)  # 40 rows of 256 values; 70 outputs
+    for dy in (x(40, 71), x(40, 128), x(39, 70), x(128, 70)):
+        with pytest.raises(ValueError, match="columns"):
+            fp8.linear_backward(dy, xt, copy, need_dx=dy.shape[1] != 70)
+
+
+def test_columns_that_a_block_matrix_does_not_have():
+    for cols in (0, -1, 128, 257):
+        with pytest.raises(ValueError, match="cols"):
+            fp8.BlockMatrix(torch.zeros(3, 256, dtype=torch.uint8),
+                            torch.zeros(3, 2, dtype=torch.uint8), "e4m3", cols=cols)
+    assert _blocks(3, 129).shape == (3, 129) and _blocks(3, 256).shape == (3, 256)
+    assert _blocks(3, 0).shape == (3, 0)

@@ -485,12 +485,33 @@ def madd_quantize_fp8(x, qfmt: str, q=None, qscale=None, qt=None, qtscale=None, 
                                        _ptr(qtscale), _stream(stream)))
 
 
+_fp8_types = {}  # torch dtype -> format of scales or codes, filled as above ("": bytes, of any)
+
+
+def _fp8_type(t):
+    if not _fp8_types:
+        for names, held in ((("uint8", "int8"), ("e8m0", "")), (("float8_e8m0fnu",), ("e8m0", None)),
+                            (("float16", "int16", "uint16"), ("fp16", None)),
+                            (("float8_e4m3fn",), (None, "e4m3")),
+                            (("float8_e5m2",), (None, "e5m2"))):
+            _fp8_types.update({torch_dtype(n): held for n in names})
+    return _fp8_types.get(t.dtype, (None, None))
+
+
 def _scale_format(what: str, t) -> str:
-    """Format of a block-scale tensor: one byte each "e8m0", two bytes "fp16"."""
-    size = t.element_size()
-    if size not in (1, 2):
+    """Format of a block-scale tensor: "e8m0" (E8M0 or its bytes) or "fp16" (FP16 or
+    its 16-bit integers)."""
+    fmt = _fp8_type(t)[0]
+    if fmt is None:
         raise TypeError(f"{what} must hold E8M0 bytes or FP16 codes (got {t.dtype})")
-    return "e8m0" if size == 1 else "fp16"
+    return fmt
+
+
+def _need_codes(what: str, t, fmt: str):
+    """A tensor of codes of this format, or of bytes."""
+    held = _fp8_type(t)[1]
+    if held != fmt and held != "":
+        raise TypeError(f"{what} must hold {fmt} codes or bytes (got {t.dtype})")
 
 
 def madd_matmul_fp8(a, afmt: str, ascale, b, bfmt: str, bscale, c, accumulate: bool = False,
@@ -504,11 +525,13 @@ def madd_matmul_fp8(a, afmt: str, ascale, b, bfmt: str, bscale, c, accumulate: b
         raise ValueError(f"{fn}: a and b must be m x k and n x k (got {tuple(a.shape)} and "
                          f"{tuple(b.shape)})")
     (m, k), n = a.shape, b.shape[0]
+    _need_codes(f"{fn}: a", a, afmt)
+    _need_codes(f"{fn}: b", b, bfmt)
     sf = _scale_format(f"{fn}: bscale", bscale)
     for name, t, nb in (("a", a, m * k), ("b", b, n * k), ("ascale", ascale, m * k // FP8_BLOCK),
                         ("bscale", bscale, n * k // FP8_BLOCK * bscale.element_size())):
         _need(f"{fn}: {name}", t, nb)
-    if ascale.element_size() != 1:
+    if _scale_format(f"{fn}: ascale", ascale) != "e8m0":
         raise TypeError(f"{fn}: a's scales must be E8M0 bytes (got {ascale.dtype})")
     ldc = _need_rows(f"{fn}: c", c, m, n)
     _need(f"{fn}: workspace", workspace, 0)
@@ -527,6 +550,7 @@ def madd_linear_fp8(x, b, bfmt: str, bscale, y, workspace=None, stream=None):
     if k != kw:
         raise ValueError(f"{fn}: x and b must be m x k and n x k (got {tuple(x.shape)} and "
                          f"{tuple(b.shape)})")
+    _need_codes(f"{fn}: b", b, bfmt)
     sf = _scale_format(f"{fn}: bscale", bscale)
     ldx, ldy = _need_rows(f"{fn}: x", x, m, k), _need_rows(f"{fn}: y", y, m, n)
     _need(f"{fn}: b", b, n * k)

@@ -42,7 +42,7 @@ class BlockMatrix:
 
     def __init__(self, codes, scales, fmt: str | None = None, shape=None, cols: int | None = None):
         named = _FMT.get(codes.dtype)
-        if named is None and (fmt not in _DTYPE or codes.element_size() != 1):
+        if named is None and (fmt not in _DTYPE or codes.dtype not in (torch.uint8, torch.int8)):
             raise TypeError("BlockMatrix: codes must be float8_e4m3fn or float8_e5m2, or bytes "
                             f"with fmt \"e4m3\" or \"e5m2\" (got {codes.dtype}, {fmt!r})")
         if named is not None and fmt not in (None, named):

@@ -127,3 +127,41 @@ def test_columns_that_a_block_matrix_does_not_have():
                             torch.zeros(3, 2, dtype=torch.uint8), "e4m3", cols=cols)
     assert _blocks(3, 129).shape == (3, 129) and _blocks(3, 256).shape == (3, 256)
     assert _blocks(3, 0).shape == (3, 0)
+
+
+def test_scales_and_codes_of_other_formats_are_refused():
+    """Types of one or two bytes that hold other values: their bits would be read as
+    E8M0, FP16 or the named FP8 format."""
+    codes, u8 = torch.zeros(3, 256, dtype=torch.uint8), torch.uint8
+    zeros = lambda dtype: torch.zeros(3, 2, dtype=dtype)  # noqa: E731
+    for good in (u8, torch.float8_e8m0fnu, torch.float16, torch.int16, torch.uint16):
+        fp8.BlockMatrix(codes, zeros(good), "e4m3")
+    for bad in (torch.bfloat16, torch.float8_e4m3fn, torch.float8_e5m2, torch.bool, torch.float32,
+                torch.int32):
+        with pytest.raises(TypeError):
+            fp8.BlockMatrix(codes, zeros(bad), "e4m3")
+    for bad in (torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.float8_e8m0fnu, torch.bool,
+                torch.int16):
+        with pytest.raises(TypeError):
+            fp8.BlockMatrix(codes.to(bad), zeros(u8), "e4m3")
+    assert fp8.BlockMatrix(codes.view(torch.int8), zeros(u8), "e5m2").fmt == "e5m2"
+
+
+def test_the_binding_refuses_codes_of_other_formats(monkeypatch):
+    monkeypatch.setattr(B, "_need", lambda *a: None)
+    monkeypatch.setattr(B, "_need_rows", lambda what, t, rows, cols: cols)
+    monkeypatch.setattr(B, "lib", lambda: pytest.fail("reached the library"))
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    c, x, s = torch.zeros(3, 4), torch.zeros(3, 128), u8(4, 1)
+    for bad in (torch.zeros(4, 128), u8(4, 128).view(torch.float8_e5m2), u8(4, 128).bool()):
+        with pytest.raises(TypeError):
+            B.madd_matmul_fp8(u8(3, 128), "e4m3", u8(3, 1), bad, "e4m3", s, c)
+        with pytest.raises(TypeError):
+            B.madd_matmul_fp8(bad[:3], "e4m3", u8(3, 1), u8(4, 128), "e4m3", s, c)
+        with pytest.raises(TypeError):
+            B.madd_linear_fp8(x, bad, "e4m3", s, c)
+    for bad in (s.view(torch.float8_e4m3fn), s.to(torch.bfloat16)):
+        with pytest.raises(TypeError):
+            B.madd_matmul_fp8(u8(3, 128), "e4m3", u8(3, 1), u8(4, 128), "e4m3", bad, c)
+        with pytest.raises(TypeError):
+            B.madd_linear_fp8(x, u8(4, 128), "e4m3", bad, c)

@@ -592,14 +592,16 @@ class GradList:
     def set(self, gs):
         gs = list(gs)
         assert len(gs) == self.n
+        formats = list(self.gfmt)
         for i, t in enumerate(gs):
             if t is not None:
                 if t.numel() != self.numel[i]:
                     raise ValueError(f"GradList[{i}] holds {t.numel()} gradients; the list was "
                                      f"made for {self.numel[i]}")
-                self.gfmt[i] = GFMT[_value_format(f"GradList[{i}]", t)]
+                formats[i] = GFMT[_value_format(f"GradList[{i}]", t)]
                 _need(f"GradList[{i}]", t, 0)
-            self.g[i] = _ptr(t)
+        # all are right: only now does anything change
+        self.g[:], self.gfmt[:] = [_ptr(t) for t in gs], formats
         self._tensors = gs
         f = set(self.gfmt)
         # the one format of every gradient, or None

@@ -48,3 +48,18 @@ def test_a_step_tells_autograd_that_the_parameters_changed(stub):
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
     loss2.backward()  # a parameter that had no gradient is as it was
+
+
+def test_refused_gradients_leave_a_list_as_it_was(stub):
+    """A list's addresses belong to tensors that it keeps alive: a set that is refused
+    half way must not leave addresses of tensors that nobody holds."""
+    a, b = torch.ones(4), torch.ones(6)
+    gl = B.GradList([a, b])
+    before = list(gl.g), list(gl.gfmt), gl.format
+    for bad in ([torch.ones(4), torch.ones(5)], [torch.ones(4).bfloat16(), torch.ones(6).double()]):
+        with pytest.raises((ValueError, TypeError)):
+            gl.set(bad)
+        assert (list(gl.g), list(gl.gfmt), gl.format) == before
+        assert gl._tensors[0] is a and gl._tensors[1] is b
+    gl.set([a.bfloat16(), None])
+    assert gl.g[0] == gl._tensors[0].data_ptr() and gl.g[1] is None

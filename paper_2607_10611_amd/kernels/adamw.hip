@@ -235,17 +235,20 @@ __device__ __forceinline__ u2 encode8(const float (&x)[8], u4 draw, uint32_t cod
 // anyway (m by 2^64, v by 2^80; r comes out 2^40 times, the quotient 2^64 times
 // larger).  Each operation stays one rounding of the same real number but
 // for a v below 2^-126 (a denormal): its root, below 2^-63, may be half
-// again too large, which is nothing beside an eps of 2^-38; where it would
-// be stored (every root of the block is small) it is taken again.  Anything
-// else outside takes the general operations: w, m or v from 2^26 on, infinities,
-// NaN, hyper-parameters beyond `usable`.
+// again too large.  `usable` sees to it that such a root, with its factor, is less
+// than half a unit in the last place of eps, so that the sum with eps is eps for
+// either root; where the root would be stored (every root of the block is small) it
+// is taken again.  Anything else outside takes the general operations: w, m or v
+// from 2^26 on, infinities, NaN, hyper-parameters beyond `usable`.
 template <bool S8>
 __device__ __forceinline__ bool adamw8(const float (&w)[8], const float (&g)[8], float (&m)[8],
                                        float (&v)[8], float (&r)[8], float (&wn)[8], float c,
                                        const AdamScalars& s) {
   using namespace madd_exact;
   const float alr = fabsf(s.lr);
+  // (1.5 2^-63 ir2 <= 0.75 2^-25 eps, half a unit of eps or less: ir2 <= 2^37 eps)
   const bool usable = s.eps >= 0x1p-38f && s.eps < 0x1p20f && s.ir2 < 0x1p20f &&
+                      s.ir2 * 0x1p-37f <= s.eps &&
                       (alr == 0.0f || (alr >= 0x1p-60f && alr < 0x1p20f));
   float hi = 0.0f;
 #pragma unroll

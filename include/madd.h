@@ -434,7 +434,10 @@ int32_t madd_quantize_fp8(const void* x, int32_t xfmt, int64_t rows, int64_t col
  *          c holds, in fp32.
  * k is a multiple of 128 (else MADD_EINVAL); k = 0 gives zeros.  a and b are
  * 16-byte aligned, c and FP16 scales to their elements (else MADD_EALIGN).
- * A NaN scale or code makes NaN of the values it enters.
+ * A NaN scale or code makes NaN of the values it enters.  Beside FP16 scales a
+ * block's sum is kept 2^-24 times as large before its scale is applied: it may pass
+ * fp32's largest value where the result does not, and rows so small that it
+ * is a denormal then lose bits below 2^-126 of the FP16 scale.
  * workspace : device memory of workspace_bytes bytes, 16-byte aligned, that the
  *          call may overwrite; madd_matmul_fp8_workspace(m, n, k) bytes serve
  *          best (-1 for a negative argument or one above 2^31).  With less, or

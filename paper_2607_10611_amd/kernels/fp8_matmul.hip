@@ -54,6 +54,16 @@ __device__ __forceinline__ f16v mfma(i8v x, i8v y, f16v c, uint32_t sx, uint32_t
                                                         (int)sx, 0, (int)sy);
 }
 
+// A block's sum that an FP16 scale will multiply is kept 2^-24 times as large, by the
+// matrix instruction's own scale of b: 128 products of the largest codes (2^31.6 for
+// E4M3 by E5M2) times a's scale pass fp32's largest value from scales of 2^97 on, rows
+// of 2^105, where the result need not.  (Below 2^-126 it loses bits instead: 2^-126 of
+// the FP16 scale at most.)  The scale takes the factor back, in its own conversion.
+constexpr uint32_t kBlockScale = 127u - 24u;
+__device__ __forceinline__ float block_scale(uint32_t fp16) {
+  return fmaf(dec_fp16(fp16), 0x1p24f, 0.0f);
+}
+
 // Four consecutive columns of a row of c, `have` of which exist.
 __device__ __forceinline__ void store_c(const MatmulArgs& p, int64_t row, int64_t col, int have,
                                         f4 x) {
@@ -315,14 +325,16 @@ void matmul_tile_kernel(MatmulArgs args) {
         if (n < HM * HN) {
           const int i = n / HN, j = n % HN;
           between(2 * n);
-          t[n % 2] = mfma<AF, BF>(a[ha][i].half(0), b[hb][j].half(0), none, sa[ha * HM + i], 127u);
+          t[n % 2] = mfma<AF, BF>(a[ha][i].half(0), b[hb][j].half(0), none, sa[ha * HM + i],
+                                  kBlockScale);
           between(2 * n + 1);
-          t[n % 2] = mfma<AF, BF>(a[ha][i].half(1), b[hb][j].half(1), t[n % 2], sa[ha * HM + i], 127u);
+          t[n % 2] = mfma<AF, BF>(a[ha][i].half(1), b[hb][j].half(1), t[n % 2], sa[ha * HM + i],
+                                  kBlockScale);
         }
         if (n > 0) {
           const int i = (n - 1) / HN, j = (n - 1) % HN;
           f16v& c = acc[ha * HM + i][hb * HN + j];
-          const float s = dec_fp16((uint32_t)sb[hb * HN + j] & 0xFFFFu);
+          const float s = block_scale((uint32_t)sb[hb * HN + j] & 0xFFFFu);
 #pragma unroll
           for (int k = 0; k < 16; ++k) c[k] = fmaf(t[(n - 1) % 2][k], s, c[k]);
         }
@@ -678,8 +690,9 @@ __global__ __launch_bounds__(64 * WAVES) void matmul_rows_kernel(MatmulArgs p, R
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
             if constexpr (SB16) {
-              const f4 t = mfma16<AF, BF>(a[u][i], b[u][j], f4{0.0f, 0.0f, 0.0f, 0.0f}, sa[u][i], 127u);
-              const float s = dec_fp16(sb[u][j]);
+              const f4 t = mfma16<AF, BF>(a[u][i], b[u][j], f4{0.0f, 0.0f, 0.0f, 0.0f}, sa[u][i],
+                                          kBlockScale);
+              const float s = block_scale(sb[u][j]);
 #pragma unroll
               for (int k = 0; k < 4; ++k) acc[i][j][k] = fmaf(t[k], s, acc[i][j][k]);
             } else {

@@ -515,7 +515,8 @@ typedef struct madd_adamw_hparams {
  *           index, which key the draws as in madd_round.
  * grad_scale : NULL, or a device float that multiplies every gradient
  *           (madd_grad_norm's coefficient).  If it is a NaN the step changes
- *           nothing.
+ *           nothing; hp->step is the caller's, who takes the same t again if such
+ *           a step is not to count.
  * Arrays are aligned to their elements (else MADD_EALIGN) and start anywhere;
  * those of a tensor must not overlap (MADD_EINVAL; g and grad_scale may).  A
  * tensor of more than (2^24 - 1) 2048 elements is MADD_EUNSUPPORTED.  Nothing is

@@ -324,7 +324,7 @@ def grad_norm(parameters, max_norm: float = math.inf):
     min(1, max_norm / norm), as two 0-dimensional GPU tensors (the host is not
     waited for).  The gradients are not changed: give the coefficient to
     AdamW.step(grad_scale=...).  It is NaN where the norm is not finite, which
-    makes that step leave everything as it is."""
+    makes that step leave the parameters and moments as they are."""
     gs = [p.grad for p in parameters if p.grad is not None]
     if not gs:
         raise ValueError("grad_norm: no parameter has a gradient")
@@ -467,8 +467,11 @@ class AdamW(torch.optim.Optimizer):
     def step(self, closure=None, grad_scale=None):
         """One step.  grad_scale: a float32 GPU tensor of one value that
         multiplies every gradient on the way (grad_norm's coefficient); a NaN
-        leaves parameters and states as they are.  A step cannot be captured in a
-        graph: its number and hyper-parameters go to the kernel by value."""
+        leaves parameters, masters, moments and scales as they are.  The host does
+        not learn of that: the state's "step" counts every call, and with it the
+        bias corrections go on.  A program that knows of a skipped step takes it
+        back with state[p]["step"] -= 1.  A step cannot be captured in a graph: its
+        number and hyper-parameters go to the kernel by value."""
         if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("AdamW: a step cannot be captured (every replay would repeat its "
                                "step number)")

@@ -1,10 +1,13 @@
 """AdamW at the ends of its range (GPU)."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2607_10611_amd import binding as B
-from test_gpu_adamw import HP, Case, check
+from paper_2607_10611_amd.optim import AdamW
+from test_gpu_adamw import HP, Case, check, params, set_grads
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +32,24 @@ def test_every_operation_is_rounded_also_where_v_is_denormal(bits, beta2, eps, s
     check(case, hp, np.float32(1.0))
     v = case.h[0][3]
     assert bits or ((v > 0) & (v < 2.0 ** -126)).any()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(rounding="sr", state_format="8bit")])
+def test_a_skipped_step_counts_until_it_is_taken_back(kw):
+    """A NaN scale keeps parameters and moments, but the host does not learn of it and
+    counts the step; a program that learns of it takes it back from the counts."""
+    runs = [params(torch.bfloat16) for _ in range(3)]
+    opts = [AdamW(p, seed=2, **kw) for p in runs]
+    nan = torch.tensor([math.nan], device="cuda")
+    for ps, o in list(zip(runs, opts))[:2]:
+        set_grads(ps, 9)
+        o.step(grad_scale=nan)
+        assert all(o.state[p]["step"] == 1 for p in ps)
+    for p in runs[0]:
+        opts[0].state[p]["step"] -= 1
+    for ps, o in zip(runs, opts):
+        set_grads(ps, 1)
+        o.step()
+    assert all(torch.equal(a, c) for a, c in zip(runs[0], runs[2]))
+    assert not all(torch.equal(b, c) for b, c in zip(runs[1], runs[2]))
+    assert [o.state[ps[0]]["step"] for ps, o in zip(runs, opts)] == [1, 2, 1]

@@ -475,6 +475,9 @@ class AdamW(torch.optim.Optimizer):
         if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("AdamW: a step cannot be captured (every replay would repeat its "
                                "step number)")
+        if grad_scale is not None and not torch.is_tensor(grad_scale):
+            raise TypeError("AdamW: grad_scale must be a float32 GPU tensor (got "
+                            f"{type(grad_scale).__name__})")
         loss = None
         if closure is not None:
             with torch.enable_grad():

@@ -63,3 +63,13 @@ def test_refused_gradients_leave_a_list_as_it_was(stub):
         assert gl._tensors[0] is a and gl._tensors[1] is b
     gl.set([a.bfloat16(), None])
     assert gl.g[0] == gl._tensors[0].data_ptr() and gl.g[1] is None
+
+
+@pytest.mark.parametrize("scale", [4, 0, 1, 0.5, True])
+def test_a_scale_that_is_no_tensor_is_refused(stub, scale):
+    """An integer would be taken for a device address."""
+    p = parameter()
+    opt = AdamW([p])
+    with pytest.raises(TypeError, match="grad_scale"):
+        opt.step(grad_scale=scale)
+    assert not stub and not opt.state[p]

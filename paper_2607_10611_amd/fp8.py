@@ -55,9 +55,9 @@ class BlockMatrix:
                              f"{B.FP8_BLOCK} (got {tuple(codes.shape)})")
         rows, k = codes.shape
         blocks = k // B.FP8_BLOCK
-        if scales.numel() != rows * blocks:
-            raise ValueError(f"BlockMatrix: {rows} x {k} codes need {rows * blocks} scales "
-                             f"(got {scales.numel()})")
+        if scales.shape not in ((rows, blocks), (rows * blocks,)):
+            raise ValueError(f"BlockMatrix: {rows} x {k} codes need {rows} x {blocks} scales "
+                             f"(got {tuple(scales.shape)})")
         B._scale_format("BlockMatrix: scales", scales)
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("BlockMatrix: codes and scales must be contiguous")

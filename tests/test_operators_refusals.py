@@ -165,3 +165,13 @@ def test_the_binding_refuses_codes_of_other_formats(monkeypatch):
             B.madd_matmul_fp8(u8(3, 128), "e4m3", u8(3, 1), u8(4, 128), "e4m3", bad, c)
         with pytest.raises(TypeError):
             B.madd_linear_fp8(x, u8(4, 128), "e4m3", bad, c)
+
+
+def test_scales_of_another_shape_are_refused():
+    """As many scales in another order, such as the transposed ones."""
+    codes = torch.zeros(4, 256, dtype=torch.uint8)
+    make = lambda *s: fp8.BlockMatrix(codes, torch.zeros(*s, dtype=torch.uint8), "e4m3")  # noqa: E731
+    for bad in ((2, 4), (1, 8), (8, 1), (4, 2, 1), (2, 2, 2)):
+        with pytest.raises(ValueError, match="scales"):
+            make(*bad)
+    assert make(4, 2).scales.shape == make(8).scales.shape == (4, 2)

@@ -490,11 +490,10 @@ _fp8_types = {}  # torch dtype -> format of scales or codes, filled as above (""
 
 def _fp8_type(t):
     if not _fp8_types:
-        for names, held in ((("uint8", "int8"), ("e8m0", "")), (("float8_e8m0fnu",), ("e8m0", None)),
-                            (("float16", "int16", "uint16"), ("fp16", None)),
-                            (("float8_e4m3fn",), (None, "e4m3")),
-                            (("float8_e5m2",), (None, "e5m2"))):
-            _fp8_types.update({torch_dtype(n): held for n in names})
+        held = {"uint8": ("e8m0", ""), "int8": ("e8m0", ""), "float8_e8m0fnu": ("e8m0", None),
+                "float16": ("fp16", None), "int16": ("fp16", None), "uint16": ("fp16", None),
+                "float8_e4m3fn": (None, "e4m3"), "float8_e5m2": (None, "e5m2")}
+        _fp8_types.update({torch_dtype(n): h for n, h in held.items()})
     return _fp8_types.get(t.dtype, (None, None))
 
 
@@ -644,6 +643,7 @@ class AdamWList:
         self.sfmt = "fp32" if scales is None else "8bit"
         self.numel = (ctypes.c_int64 * k)(*[t.numel() for t in ws])
         wb, sb = GRAD_BYTES[self.wfmt], 4 if scales is None else 1
+        copy_types = [torch_dtype(t) for t in ("bfloat16", "int16", "uint16")]
         for i in range(k):
             n = ws[i].numel()
             if _value_format(f"AdamWList[{i}]: w", ws[i]) != self.wfmt:
@@ -655,8 +655,14 @@ class AdamWList:
                                     f"(got {t.dtype})")
                 _need(f"AdamWList[{i}]: {name}", t, n * sb)
             if scales is not None:
+                if _fp8_type(scales[i])[0] != "e8m0":
+                    raise TypeError(f"AdamWList[{i}]: scales must be E8M0 bytes (got "
+                                    f"{scales[i].dtype})")
                 _need(f"AdamWList[{i}]: scales", scales[i], 2 * -(-n // FP8_BLOCK))
             if copies is not None and copies[i] is not None:
+                if copies[i].dtype not in copy_types:
+                    raise TypeError(f"AdamWList[{i}]: a copy must be bfloat16 or 16-bit integers "
+                                    f"(got {copies[i].dtype})")
                 _need(f"AdamWList[{i}]: copy", copies[i], 2 * n)
         Arr = ctypes.c_void_p * k
         self._tensors = [list(ws), list(ms), list(vs), list(scales or []), list(copies or [])]

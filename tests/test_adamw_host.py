@@ -73,3 +73,18 @@ def test_a_scale_that_is_no_tensor_is_refused(stub, scale):
     with pytest.raises(TypeError, match="grad_scale"):
         opt.step(grad_scale=scale)
     assert not stub and not opt.state[p]
+
+
+def test_copies_and_scales_of_other_types_are_refused(stub):
+    """bf16 codes would be written into a float16 copy, scale bytes over floats."""
+    f, u8 = torch.zeros(128), torch.zeros(128, dtype=torch.uint8)
+    for good in (torch.bfloat16, torch.int16, torch.uint16):
+        B.AdamWList([f], [f], [f], [f], copies=[f.to(good)])
+    for bad in (torch.float16, torch.float32, torch.int32):
+        with pytest.raises(TypeError, match="copy"):
+            B.AdamWList([f], [f], [f], [f], copies=[f.to(bad)])
+    for good in (torch.uint8, torch.int8, torch.float8_e8m0fnu):
+        B.AdamWList([f], [f], [u8], [u8], scales=[torch.zeros(2).to(good)])
+    for bad in (torch.float16, torch.float32, torch.float8_e4m3fn):
+        with pytest.raises(TypeError, match="scales"):
+            B.AdamWList([f], [f], [u8], [u8], scales=[torch.zeros(2).to(bad)])

@@ -48,7 +48,7 @@ _HP_KEYS = ("lr_add", "lr_mul", "eps", "tau", "r_max", "eps0", "g_max", "d_mult_
 def was_replaced(t) -> bool:
     """Whether t is, or is a view of, master codes or scales that are no longer
     an optimizer's because MAdam.load_state_dict put others in their place."""
-    return t in _replaced or (t._base is not None and t._base in _replaced)
+    return bool(_replaced) and (t in _replaced or (t._base is not None and t._base in _replaced))
 
 
 class MAdam(torch.optim.Optimizer):
